@@ -42,6 +42,7 @@ struct RotaryParams {
 // One lane's eight channels of a head: two runs of four (neighbours, or from the two halves of the rotated channels).
 struct Lane {
   int c0, c1;                        // first channels of the runs
+  int turned;                        // its pairs below this are turned, the others pass as they are
   float cs[4], sn[4];
 };
 
@@ -52,6 +53,7 @@ __device__ __forceinline__ Lane lane_of(const RotaryParams& p, int j, const void
   const bool split = p.halves && 4 * j < half;
   l.c0 = split ? 4 * j : 8 * j;
   l.c1 = split ? half + 4 * j : 8 * j + 4;
+  l.turned = half - 4 * j;
   // All positions of the token are read, and the lane's pairs pick theirs: no read waits for another.
   double at[kMaxAxes];
 #pragma unroll
@@ -64,7 +66,7 @@ __device__ __forceinline__ Lane lane_of(const RotaryParams& p, int j, const void
     const int pair = min(4 * j + i, kMaxPairs - 1), a = p.axis[pair];
     const double here = a == 0 ? at[0] : a == 1 ? at[1] : a == 2 ? at[2] : at[3];
     // whole revolutions are dropped in 64 bits: positions are few bits, so the angle is as exact as its frequency
-    const double rev = here * p.turns[pair];             // 0 for a pair that is not turned
+    const double rev = here * p.turns[pair];
     sincospif(2.f * (float)(rev - rint(rev)), &l.sn[i], &l.cs[i]);
   }
   return l;
@@ -95,19 +97,15 @@ __device__ __forceinline__ void load_weight(const __bf16* w, const Lane& l, floa
     v[e + 4] = (float)w[l.c1 + e];
   }
 }
-// rotation by +1 or -1 times the angle
+// rotation by +1 or -1 times the angle; a channel that is not turned takes nothing from its neighbour, which may be infinite
 __device__ __forceinline__ void turn(const Lane& l, bool halves, float sign, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float a = halves ? v[i] : v[2 * i], b = halves ? v[i + 4] : v[2 * i + 1];
+    const float a = halves ? v[i] : v[2 * i], b = halves ? v[i + 4] : v[2 * i + 1];
     const float s = sign * l.sn[i], x = a * l.cs[i] - b * s, y = a * s + b * l.cs[i];
-    if (halves) {
-      v[i] = x;
-      v[i + 4] = y;
-    } else {
-      v[2 * i] = x;
-      v[2 * i + 1] = y;
-    }
+    const bool on = i < l.turned;
+    v[halves ? i : 2 * i] = on ? x : a;
+    v[halves ? i + 4 : 2 * i + 1] = on ? y : b;
   }
 }
 
