@@ -65,8 +65,8 @@ extern "C" {
  *   O            device, bf16 [B,H,L,D], written (computed blocks always; cached blocks only
  *                when O_cache is a different tensor).  Must not overlap Q, K or V.
  * The call is asynchronous with respect to the host.  It uses a per (device, stream) scratch
- * buffer that the library allocates on first use and grows when needed (hipMalloc); calls that
- * overlap in time on one stream object are not supported.
+ * buffer that the library allocates on first use and grows when needed (hipMalloc).  Host threads may call on one stream
+ * at the same time: a call that needs the buffer waits until another's kernels are enqueued.
  */
 int sparse_attn_fwd(const void* Q, const void* K, const void* V,
                     const uint8_t* cache_flags, const uint8_t* kv_mask,
@@ -333,7 +333,8 @@ int sparse_attn_profile_end(int* calls, double* plan_ms_total, double* attn_ms_t
  * sparse_attn_fwd_forecast and sparse_symbols_update* keep one device buffer per (device, stream) inside the
  * library: allocated on the first call on that stream (hipMalloc), grown when a later call needs more (stream
  * synchronisation + hipFree + hipMalloc), shared by all of these calls on the stream, never shrunk.  Consequences:
- * such a call can be captured into a HIP graph only after a call of at least the same size has run on that stream,
+ * calls of several host threads on one stream wait for each other (while the other's kernels are enqueued, not while they
+ * run); such a call can be captured into a HIP graph only after a call of at least the same size has run on that stream,
  * and a graph captured from it becomes invalid if the buffer grows afterwards; the plan calls, sparse_attn_fwd_noalloc
  * and sparse_attn_fwd_workspace have no such restriction.  sparse_attn_release_scratch waits for the stream and frees
  * its buffer (call it before destroying a stream: the library cannot see that a stream handle has died, and a

@@ -1299,12 +1299,7 @@ size_t workspace_bytes(const Shape& s) {
   return kQueueBytes + align256((size_t)s.N * 8) + align256((size_t)s.N * 4) + align256((size_t)s.N * s.nw32 * 4);
 }
 
-struct Scratch {
-  void* ptr = nullptr;
-  size_t bytes = 0;
-};
 std::mutex g_mu;
-std::map<std::pair<int, void*>, Scratch> g_scratch;
 
 }  // namespace
 
@@ -1339,23 +1334,57 @@ int static_scratch_ptr(void** out) {
 
 }  // namespace
 
-int sa_get_scratch(size_t need, hipStream_t stream, void** out) {
+struct sa_scratch::Buffer {
+  std::mutex mu;           // held by the call that uses the buffer
+  void* ptr = nullptr;
+  size_t bytes = 0;
+};
+
+// NULL without host memory.  Entries stay, empty ones too: a thread may be waiting for one.
+sa_scratch::Buffer* sa_scratch::of(int dev, hipStream_t stream) {
+  static std::map<std::pair<int, void*>, Buffer> buffers;
+  std::lock_guard<std::mutex> lock(g_mu);
+  try {
+    return &buffers[std::make_pair(dev, (void*)stream)];
+  } catch (const std::bad_alloc&) {
+    return nullptr;
+  }
+}
+
+int sa_scratch::get(size_t need, hipStream_t stream) {
   int dev = 0;
   HIP_TRY(hipGetDevice(&dev));
-  std::lock_guard<std::mutex> lock(g_mu);
-  Scratch& sc = g_scratch[std::make_pair(dev, (void*)stream)];
-  if (sc.bytes < need) {
-    if (sc.ptr) {
+  held_ = of(dev, stream);
+  if (!held_) return sa_fail(SPARSE_ATTN_ERR_HIP, "out of host memory");
+  held_->mu.lock();
+  if (held_->bytes < need) {
+    if (held_->ptr) {
       HIP_TRY(hipStreamSynchronize(stream));
-      HIP_TRY(hipFree(sc.ptr));
-      sc.ptr = nullptr;
-      sc.bytes = 0;
+      HIP_TRY(hipFree(held_->ptr));
+      held_->ptr = nullptr;
+      held_->bytes = 0;
     }
     const size_t want = need + need / 2;
-    HIP_TRY(hipMalloc(&sc.ptr, want));
-    sc.bytes = want;
+    HIP_TRY(hipMalloc(&held_->ptr, want));
+    held_->bytes = want;
   }
-  *out = sc.ptr;
+  ptr_ = (char*)held_->ptr;
+  return 0;
+}
+
+sa_scratch::~sa_scratch() {
+  if (held_) held_->mu.unlock();
+}
+
+int sa_release_scratch(hipStream_t stream) {
+  sa_scratch scratch;
+  if (int rc = scratch.get(0, stream)) return rc;
+  if (scratch.data()) {
+    HIP_TRY(hipStreamSynchronize(stream));    // work that still uses the buffer
+    HIP_TRY(hipFree(scratch.data()));
+    scratch.held_->ptr = nullptr;
+    scratch.held_->bytes = 0;
+  }
   return 0;
 }
 
@@ -1520,6 +1549,7 @@ int run(const void* Q, const void* K, const void* V, const uint8_t* cache_flags,
   if (plan && dev != plan->dev) return fail(SPARSE_ATTN_ERR_INVALID, "the plan was created on device %d, current device is %d", plan->dev, dev);
 
   PlanBuffers pb;
+  sa_scratch scratch;
   if (plan) {
     pb = plan->bufs;
   } else if (use_user_ws) {
@@ -1529,9 +1559,8 @@ int run(const void* Q, const void* K, const void* V, const uint8_t* cache_flags,
     if (int rc = static_scratch_ptr(&ws)) return rc;
     pb = carve((char*)ws, s);
   } else {
-    void* ws = nullptr;
-    if (int rc = sa_get_scratch(workspace_bytes(s), stream, &ws)) return rc;
-    pb = carve((char*)ws, s);
+    if (int rc = scratch.get(workspace_bytes(s), stream)) return rc;
+    pb = carve(scratch.data(), s);
   }
 
   HIP_TRY(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
@@ -1764,23 +1793,7 @@ int sparse_attn_fwd_workspace(const void* Q, const void* K, const void* V, const
              nullptr, false, nullptr, nullptr, false, workspace, workspace_size, true);
 }
 
-int sparse_attn_release_scratch(void* hip_stream) {
-  int dev = 0;
-  HIP_TRY(hipGetDevice(&dev));
-  void* ptr = nullptr;
-  {
-    std::lock_guard<std::mutex> lock(g_mu);
-    auto it = g_scratch.find(std::make_pair(dev, hip_stream));
-    if (it == g_scratch.end()) return 0;
-    ptr = it->second.ptr;
-    g_scratch.erase(it);
-  }
-  if (ptr) {
-    HIP_TRY(hipStreamSynchronize((hipStream_t)hip_stream));    // work that still uses the buffer
-    HIP_TRY(hipFree(ptr));
-  }
-  return 0;
-}
+int sparse_attn_release_scratch(void* hip_stream) { return sa_release_scratch((hipStream_t)hip_stream); }
 
 size_t sparse_attn_workspace_bytes(int B, int H, int L, int block_q, int block_k) {
   Shape s;

@@ -9,10 +9,28 @@
 // Records a printf-style message for sparse_attn_last_error() on the calling thread and returns `code`.
 int sa_fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 
-// The library's scratch buffer of the current device and `stream`, grown (with a stream synchronisation) to at
-// least `need` bytes.  Every entry point that needs scratch memory shares it: work on one stream runs in
-// order, and no entry point keeps anything in it between calls.
-int sa_get_scratch(size_t need, hipStream_t stream, void** out);
+// The library's scratch buffer of the current device and a stream.  Every entry point that needs scratch memory shares it:
+// work on one stream runs in order, and no entry point keeps anything in it between calls.  A call's kernels hand each other
+// operands in it, so the object has to live until the last of them is enqueued: until then no other thread's call on the
+// stream gets the buffer, to write to it between them or to replace it.
+class sa_scratch {
+ public:
+  sa_scratch() = default;
+  sa_scratch(const sa_scratch&) = delete;
+  sa_scratch& operator=(const sa_scratch&) = delete;
+  ~sa_scratch();
+  // Takes the buffer, grown (with a stream synchronisation) to at least `need` bytes.  Once in the object's life.
+  int get(size_t need, hipStream_t stream);
+  char* data() const { return ptr_; }
+
+ private:
+  struct Buffer;
+  static Buffer* of(int dev, hipStream_t stream);
+  friend int sa_release_scratch(hipStream_t stream);
+  Buffer* held_ = nullptr;
+  char* ptr_ = nullptr;
+};
+int sa_release_scratch(hipStream_t stream);
 
 // Direct-to-LDS load: every lane fetches 16 bytes from gbase (wave-uniform) + lane_off, the wave's
 // 1 KiB lands at consecutive LDS addresses starting at the wave-uniform `lds_addr`.  Written as

@@ -740,16 +740,16 @@ int sparse_block_norm_backward(const sparse_block_norm_backward_args* a, void* h
   const size_t extra = vectors > 1 ? (size_t)vectors * C : 0;
   const int runs = chunks > kFold ? (int)((chunks + kFold - 1) / kFold) : 0;
   const size_t folded = (size_t)vectors * runs * C;
-  void* scratch = nullptr;
+  sa_scratch scratch;
   if (want_s || want_a || want_e)
-    if (int rc = sa_get_scratch((3 * plane + 2 * extra + 3 * folded) * 4, stream, &scratch)) return rc;
-  float* part = (float*)scratch;
+    if (int rc = scratch.get((3 * plane + 2 * extra + 3 * folded) * 4, stream)) return rc;
+  float* part = (float*)scratch.data();
   BackParams p = {a->dh, a->dx_out, a->x_out, a->y, a->weight, a->scale, a->gate, a->post_weight, a->dx, a->dy, part, a->rows,
                   a->rows_per_vector, vectors, a->scale_stride, a->gate_stride, C, a->norm == SPARSE_BLOCK_NORM_LAYER, (int)chunks, (int)per, 0,
                   want_s, want_a, want_e, a->y ? a->alpha : 1.f, a->eps, a->post_eps};
   by_types(a->x_dtype, a->vector_dtype, [&](auto tx, auto tv) { launch_backward<decltype(tx), decltype(tv)>(p, vec, stream); });
   if (int rc = launched(who)) return rc;
-  if (!scratch) return 0;
+  if (!part) return 0;
   float* wa = !a->dweight ? nullptr : vectors > 1 ? part + 3 * plane : a->dweight;
   float* we = !a->dpost_weight ? nullptr : vectors > 1 ? part + 3 * plane + extra : a->dpost_weight;
   FinishParams f = {part, part + 3 * plane + 2 * extra, a->weight, a->scale, a->gate, a->post_weight, a->dscale, a->dshift, a->dgate, wa, we, vectors,

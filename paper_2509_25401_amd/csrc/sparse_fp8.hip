@@ -1053,10 +1053,10 @@ int sparse_fp8_gemm(const void* a, const uint8_t* a_scales, int a_block, const v
   const GemmParams p = {(const uint8_t*)a, a_scales, (const uint8_t*)b, b_scales, (const __bf16*)bias, out, M, N, K, K, (int)K, groups,
                         a_block ? 7 : 0, b_block ? 7 : 0, size == 4};
   const Route r = route_of(M, N, groups);
-  void* scratch = nullptr;
+  sa_scratch scratch;
   if (r.scratch)
-    if (int rc = sa_get_scratch(r.scratch, (hipStream_t)hip_stream, &scratch)) return rc;
-  return launch_gemm(who, p, r, (uint8_t*)scratch, (hipStream_t)hip_stream);
+    if (int rc = scratch.get(r.scratch, (hipStream_t)hip_stream)) return rc;
+  return launch_gemm(who, p, r, (uint8_t*)scratch.data(), (hipStream_t)hip_stream);
 }
 
 int sparse_fp8_linear(const void* x, const void* w, const uint8_t* w_scales, const void* bias, void* out, int out_dtype, long long M, long long N,
@@ -1073,11 +1073,11 @@ int sparse_fp8_linear(const void* x, const void* w, const uint8_t* w_scales, con
                              {"w_scales", w_scales, (size_t)ceil_div(N, kGroup) * groups}}))
     return rc;
   hipStream_t stream = (hipStream_t)hip_stream;
-  void* scratch = nullptr;
+  sa_scratch scratch;
   const Route r = route_of(M, N, groups);
   const size_t held = rounded((size_t)M * K), scaled = rounded((size_t)M * groups);
-  if (int rc = sa_get_scratch(held + scaled + r.scratch, stream, &scratch)) return rc;
-  uint8_t *x8 = (uint8_t*)scratch, *xs = x8 + held;
+  if (int rc = scratch.get(held + scaled + r.scratch, stream)) return rc;
+  uint8_t *x8 = (uint8_t*)scratch.data(), *xs = x8 + held;
   launch_quantize({(const __bf16*)x, x8, xs, nullptr, nullptr, nullptr, M, K, 0}, false, stream);
   const GemmParams p = {x8, xs, (const uint8_t*)w, w_scales, (const __bf16*)bias, out, M, N, K, K, (int)K, groups, 0, 7, size == 4};
   return launch_gemm(who, p, r, xs + scaled, stream);
@@ -1115,9 +1115,9 @@ int sparse_fp8_linear_backward(const void* dy, const void* x, const void* wt, co
   const size_t at_dy = take(dx, (size_t)M * N), at_dys = take(dx, (size_t)M * groups_n), at_dyt = take(dw, (size_t)N * pitch),
                at_dyts = take(dw, (size_t)N * groups_m), at_xt = take(dw, (size_t)K * pitch), at_xts = take(dw, (size_t)K * groups_m),
                at_part = take(dbias, (size_t)groups_m * N * 4), at_x = take(dx, rx.scratch), at_w = take(dw, rw.scratch);
-  void* scratch = nullptr;
-  if (int rc = sa_get_scratch(need, stream, &scratch)) return rc;
-  uint8_t* base = (uint8_t*)scratch;
+  sa_scratch scratch;
+  if (int rc = scratch.get(need, stream)) return rc;
+  uint8_t* base = (uint8_t*)scratch.data();
   float* part = dbias ? (float*)(base + at_part) : nullptr;
   launch_quantize({(const __bf16*)dy, dx ? base + at_dy : nullptr, dx ? base + at_dys : nullptr, dw ? base + at_dyt : nullptr,
                    dw ? base + at_dyts : nullptr, part, M, N, pitch}, false, stream);

@@ -469,10 +469,10 @@ int sparse_rotary_heads_backward(const sparse_rotary_args* a, void* dqkv, long l
   const dim3 grid((unsigned)groups, (unsigned)((heads + p.heads_per_part - 1) / p.heads_per_part));
   hipStream_t stream = (hipStream_t)hip_stream;
   const size_t n = (size_t)grid.x * grid.y;
+  sa_scratch scratch;
   if (sums) {
-    void* scratch = nullptr;
-    if (int rc = sa_get_scratch(n * 2 * a->D * 4, stream, &scratch)) return rc;
-    p.part = (float*)scratch;
+    if (int rc = scratch.get(n * 2 * a->D * 4, stream)) return rc;
+    p.part = (float*)scratch.data();
   }
   by_shape(a->D, p.halves, [&](auto d, auto h) {
     hipLaunchKernelGGL((rotary_backward_kernel<decltype(d)::value, decltype(h)::value>), grid, dim3(256), 0, stream, p);

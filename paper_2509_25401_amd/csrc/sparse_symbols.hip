@@ -635,11 +635,11 @@ int sparse_symbols_update_granular(const void* Q, const void* K, uint8_t* cache_
   const size_t pooled_b = align256((size_t)(n_q_blocks + n_k_blocks) * D * 4);
   const size_t rows_b = align256((size_t)BH * n_tq * Tk * 4);
   const size_t cols_b = align256((size_t)BH * Tq * n_tk * 4);
-  void* ws = nullptr;
-  if (int rc = sa_get_scratch(pooled_b + rows_b + cols_b, stream, &ws)) return rc;
-  float* pooled = (float*)ws;
-  float* text_rows = (float*)((char*)ws + pooled_b);
-  float* text_cols = (float*)((char*)ws + pooled_b + rows_b);
+  sa_scratch scratch;
+  if (int rc = scratch.get(pooled_b + rows_b + cols_b, stream)) return rc;
+  float* pooled = (float*)scratch.data();
+  float* text_rows = (float*)(scratch.data() + pooled_b);
+  float* text_cols = (float*)(scratch.data() + pooled_b + rows_b);
 
   const int row_bytes = (Tk + 7) / 8;
   const float scale = (float)(1.0 / sqrt((double)D));
