@@ -281,48 +281,78 @@ int check_view(const char* who, const View& v) {
   return 0;
 }
 
-// a written view must not hold an element twice: the strides, from the least, have to step over what lies inside them
+// Steps of one loop over the rows of two views: `range` values from 0 on, each `step` elements further (from `at` on, over all steps).
+struct Walk {
+  long long step, range;
+};
+
+// Whether a value of  at + sum of steps  lies in (-D, D), that is, whether two rows of D channels share an element.  The walks are
+// sorted by their span; what the later ones can still add bounds the values of the first, so that few are looked at in views that
+// are slices of one another.  `tries` bounds the others: without an answer by then the views count as overlapping.
+bool meets(const Walk* w, int n, long long at, int D, long long rest, int& tries) {
+  if (n == 0) return at > -D && at < D;
+  const long long step = w->step, after = rest - step * (w->range - 1);
+  // the values v with  -D < at + v step + [0, after] < D
+  const long long low = -D - at - after, high = D - at;                     // of v step, both excluded
+  const long long v0 = low < 0 ? 0 : low / step + 1, v1 = high <= 0 ? -1 : (high - 1) / step;
+  for (long long v = v0; v <= v1 && v < w->range; ++v) {
+    if (--tries < 0 || meets(w + 1, n - 1, at + v * step, D, after, tries)) return true;
+  }
+  return false;
+}
+
+// The differences of rows of views: walks in the order that meets() wants.
+struct Walks {
+  Walk w[6];
+  int n = 0;
+  void add(long long step, long long range) {
+    if (range <= 1 || !step) return;
+    int i = n++;
+    for (; i > 0 && w[i - 1].step < step; --i) w[i] = w[i - 1];
+    w[i] = {step, range};
+  }
+  bool meet(long long at, int D) const {
+    long long reach = 0;
+    for (int i = 0; i < n; ++i) reach += w[i].step * (w[i].range - 1);
+    int tries = 1 << 16;
+    return meets(w, n, at, D, reach, tries);
+  }
+};
+
+// a written view must not hold an element twice
 int check_written(const char* who, const View& v, int B, int L, int D) {
-  long long n[3] = {L, v.heads, B}, s[3] = {v.l, v.h, v.b};
-  for (int i = 0; i < 3; ++i)
-    for (int j = i + 1; j < 3; ++j)
-      if (s[j] < s[i]) {
-        std::swap(s[i], s[j]);
-        std::swap(n[i], n[j]);
-      }
-  long long reach = D;
-  for (int i = 0; i < 3; ++i) {
-    if (n[i] == 1) continue;
-    if (s[i] < reach) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: rows of %s overlap each other", who, v.name);
-    reach += (n[i] - 1) * s[i];
+  const long long s[3] = {v.b, v.h, v.l}, n[3] = {B, v.heads, L};
+  for (int i = 0; i < 3; ++i) {                  // two rows that differ in dimension i, maybe in those behind it, in none before it
+    if (n[i] <= 1) continue;
+    Walks d;
+    long long at = s[i];
+    d.add(s[i], n[i] - 1);
+    for (int j = i + 1; j < 3; ++j) {
+      at -= s[j] * (n[j] - 1);
+      d.add(s[j], 2 * n[j] - 1);
+    }
+    if (d.meet(at, D)) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: rows of %s overlap each other", who, v.name);
   }
   return 0;
 }
 
-// Two written views may be interleaved (slices of one tensor): they overlap only if they are the same rows; a view that
-// starts inside the other's span is told apart by its distance modulo the common token stride.
+// Two written views may be interleaved (slices of one tensor): whether a row of one shares elements with a row of the other.
 bool rows_clash(const View& a, const View& b, int B, int L, int D) {
   if (!a.p || !b.p || !overlap(a.p, view_bytes(a, B, L, D), b.p, view_bytes(b, B, L, D))) return false;
-  if (a.b == b.b && a.h == b.h && a.l == b.l) {
-    const long long away = llabs((const char*)a.p - (const char*)b.p) / 2;
-    // every stride larger than both views' reach inside it: disjoint when the offset clears the smaller strides' extent
-    long long s[3] = {a.l, a.h, a.b}, n[3] = {L, a.heads > b.heads ? a.heads : b.heads, B};
-    for (int i = 0; i < 3; ++i)
-      for (int j = i + 1; j < 3; ++j)
-        if (s[j] < s[i]) {
-          std::swap(s[i], s[j]);
-          std::swap(n[i], n[j]);
-        }
-    long long reach = D;
-    for (int i = 0; i < 3; ++i) {
-      if (n[i] > 1) {
-        const long long room = s[i], off = away % room;
-        if (away < room && off >= reach && off + reach <= room) return false;
-        reach += (n[i] - 1) * s[i];
-      }
+  Walks d;
+  long long at = (long long)((intptr_t)b.p - (intptr_t)a.p) / 2;
+  const long long sa[3] = {a.b, a.h, a.l}, sb[3] = {b.b, b.h, b.l};
+  const long long na[3] = {B, a.heads, L}, nb[3] = {B, b.heads, L};
+  for (int i = 0; i < 3; ++i) {                  // row of b minus row of a: na - 1 steps down, nb - 1 steps up
+    at -= sa[i] * (na[i] - 1);
+    if (sa[i] == sb[i]) {
+      d.add(sa[i], na[i] + nb[i] - 1);
+    } else {
+      d.add(sa[i], na[i]);
+      d.add(sb[i], nb[i]);
     }
   }
-  return true;
+  return d.meet(at, D);
 }
 
 int check_rotary(const char* who, const sparse_rotary_args* a, RotaryParams& p) {

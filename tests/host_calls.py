@@ -141,5 +141,18 @@ def threads(kind, sizes):
     return alone, lib.take()
 
 
+def rotary_views(cases):
+    """For each case (sizes, and for Q, K, V the first element and the strides of batches, heads and tokens inside one tensor): 0 where
+    the forward call takes it, else the message."""
+    lib, out = Library(), []
+    for sizes, views in cases:
+        kw = {}
+        for t, (first, b, h, l) in zip("qkv", views):
+            kw.update({t.upper(): at(2) + 2 * first, f"{t}_stride_b": b, f"{t}_stride_h": h, f"{t}_stride_l": l})
+        rc = lib.rotary(*sizes, **kw)
+        out.append(lib.error() if rc else int(any(e[1] == "launch" for e in lib.take())) - 1)
+    return out
+
+
 if __name__ == "__main__":
     print(json.dumps(globals()[sys.argv[1]](*json.loads(sys.argv[2]))))

@@ -75,3 +75,20 @@ def test_positions_that_are_no_numbers_reach_the_turned_channels_alone(D, axes, 
         t = t.cpu()
         assert torch.equal(t[..., R:], heads[:, i * H:(i + 1) * H, :, R:]), "a passing channel has changed"
         assert torch.equal(t[..., :R].isnan(), bad.expand(B, H, L, R)), "NaN in other places"
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(6, 2), (5, 1), (2, 3)])
+def test_grouped_heads_as_slices_of_one_tensor(Hq, Hkv):
+    print(f"[case] rotary slices {Hq} {Hkv}", flush=True)
+    B, L, D, axes = 2, 37, 64, (16, 24, 24)
+    g = torch.Generator().manual_seed(Hq)
+    qkv = torch.randn(B, L, (Hq + 2 * Hkv) * D, generator=g).bfloat16().cuda()
+    pos = torch.randint(0, 99, (L, 3), generator=g, dtype=torch.int32).cuda()
+    apart = [torch.zeros(B, n, L, D, dtype=torch.bfloat16, device="cuda") for n in (Hq, Hkv, Hkv)]
+    pkg.sparse_rotary_heads(qkv, pos, *apart, axes=axes)
+    want = torch.cat(apart, dim=1)
+    heads = torch.zeros(B, Hq + 2 * Hkv, L, D, dtype=torch.bfloat16, device="cuda")
+    tokens = torch.zeros(B, L, Hq + 2 * Hkv, D, dtype=torch.bfloat16, device="cuda")
+    for whole in (heads, tokens.transpose(1, 2)):
+        pkg.sparse_rotary_heads(qkv, pos, whole[:, :Hq], whole[:, Hq:Hq + Hkv], whole[:, Hq + Hkv:], axes=axes)
+        assert torch.equal(whole, want)
