@@ -2,6 +2,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "sparse_attn.h"
 #include "sparse_attn_internal.h"
 #include "sparse_block.h"
@@ -594,6 +596,12 @@ int check_overlaps(const char* who, const Range* outs, int n_out, const Range* i
   return 0;
 }
 
+int check_elements(const char* who, std::initializer_list<const void*> tensors, size_t size) {
+  for (const void* p : tensors)
+    if ((uintptr_t)p & (size - 1)) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: tensors must be aligned to their elements", who);
+  return 0;
+}
+
 template <class TX, class TV>
 void launch_norm(const NormParams& p, bool vec, bool f8, hipStream_t stream) {
   const int vectors = (p.C + 7) / 8;
@@ -682,8 +690,9 @@ int sparse_block_norm(const sparse_block_norm_args* a, void* hip_stream) {
                        {"post_weight", a->post_weight, (size_t)a->channels * vs}, {"scale", a->scale, vec_bytes(a->scale_stride)},
                        {"shift", a->shift, vec_bytes(a->shift_stride)}, {"gate", a->gate, vec_bytes(a->gate_stride)}};
   if (int rc = check_overlaps(who, outs, 3, ins, 7, a->x, a->x_out)) return rc;
-  for (const void* q : {a->x, (const void*)a->x_out, a->y, (const void*)(f8 ? nullptr : a->h), a->weight, a->post_weight, a->scale, a->shift, a->gate})
-    if ((uintptr_t)q & 1) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: tensors must be aligned to their elements", who);
+  if (int rc = check_elements(who, {a->x, a->x_out}, xs)) return rc;
+  if (int rc = check_elements(who, {a->y, f8 ? nullptr : a->h}, 2)) return rc;
+  if (int rc = check_elements(who, {a->weight, a->post_weight, a->scale, a->shift, a->gate}, vs)) return rc;
   bool vec = a->channels % 8 == 0 && aligned16(a->x) && aligned16(a->x_out) && aligned16(a->y) && aligned16(a->weight) &&
              aligned16(a->post_weight) && aligned16(a->scale) && aligned16(a->shift) && aligned16(a->gate) &&
              (a->scale_stride | a->shift_stride | a->gate_stride) % 8 == 0;
@@ -718,8 +727,10 @@ int sparse_block_norm_backward(const sparse_block_norm_backward_args* a, void* h
                        {"weight", a->weight, (size_t)C * vs}, {"post_weight", a->post_weight, (size_t)C * vs},
                        {"scale", a->scale, vec_bytes(a->scale_stride)}, {"gate", a->gate, vec_bytes(a->gate_stride)}};
   if (int rc = check_overlaps(who, outs, 7, ins, 8, a->dx_out, a->dx)) return rc;
-  for (const void* q : {a->dh, a->dx_out, a->x_out, a->y, (const void*)a->dx, (const void*)a->dy, a->weight, a->scale, a->gate, a->post_weight})
-    if ((uintptr_t)q & 1) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: tensors must be aligned to their elements", who);
+  if (int rc = check_elements(who, {a->dx_out, a->x_out, a->dx}, xs)) return rc;
+  if (int rc = check_elements(who, {a->dh, a->y, a->dy}, 2)) return rc;
+  if (int rc = check_elements(who, {a->weight, a->scale, a->gate, a->post_weight}, vs)) return rc;
+  if (int rc = check_elements(who, {a->dweight, a->dscale, a->dshift, a->dgate, a->dpost_weight}, 4)) return rc;
   const bool vec = C % 8 == 0 && aligned16(a->dh) && aligned16(a->dx_out) && aligned16(a->x_out) && aligned16(a->y) && aligned16(a->dx) &&
                    aligned16(a->dy) && aligned16(a->weight) && aligned16(a->scale) && aligned16(a->gate) && aligned16(a->post_weight) &&
                    (a->scale_stride | a->gate_stride) % 8 == 0;

@@ -472,6 +472,8 @@ int sparse_rotary_heads_backward(const sparse_rotary_args* a, void* dqkv, long l
     return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: dqkv and the gradients Q, K, V must not be NULL", who);
   if ((a->q_weight || a->k_weight) && !a->qkv) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: with a norm weight qkv must not be NULL", who);
   if ((dq_weight && !a->q_weight) || (dk_weight && !a->k_weight)) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: a weight's gradient needs the weight", who);
+  for (const void* w : {dq_weight, dk_weight})
+    if ((uintptr_t)w & 3) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: the weights' gradients must be aligned to their elements", who);
   const int heads = a->heads_q + 2 * a->heads_kv;
   const View out = {"dqkv", dqkv, dqkv_stride_b, a->D, dqkv_stride_l, heads};
   const View in[4] = {{"qkv", a->qkv, a->qkv_stride_b, a->D, a->qkv_stride_l, heads},
