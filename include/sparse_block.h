@@ -174,7 +174,7 @@ void sparse_rotary_frequencies(int axes, const int* axis_channels, double theta,
  *   qt         device, the form of the transposed matrix: row c, q_t_pitch bytes apart (a multiple of 16), holds column
  *              c, with groups along the rows of x; bytes from `rows` to the next multiple of 16 are written as zero.  Or NULL
  *   qt_scales  device, uint8 [cols, ceil(rows / 128)], block: [ceil(cols / 128), ceil(rows / 128)]; NULL with qt
- * One pass over x, whatever is asked for.  q is 16-byte aligned if cols is a multiple of 16, else any.  Any rows, cols >= 1.
+ * One pass over x, whatever is asked for.  q is 8-byte aligned if cols is a multiple of 8, else any.  Any rows, cols >= 1.
  */
 int sparse_fp8_quantize(const void* x, void* q, uint8_t* q_scales, void* qt, uint8_t* qt_scales, long long qt_pitch,
                         long long rows, long long cols, int block, void* hip_stream);

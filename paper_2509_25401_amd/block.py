@@ -382,8 +382,8 @@ def sparse_fp8_quantize(x, q=None, q_scales=None, qt=None, qt_scales=None, block
     """8-bit form of x (bf16 [R,C]): e4m3 values and exponent bytes, q * 2^(scale - 127), for groups of 128.
 
     q float8_e4m3fn [R,C] with q_scales uint8 [R,ceil(C/128)] (groups along a row), and / or the transposed form qt [C,R] with
-    qt_scales [C,ceil(R/128)] (groups along the rows of x; the rows of qt may be further apart than R, at a multiple of 16
-    bytes).  block=True: groups of 128 x 128, scales [ceil(R/128),ceil(C/128)] and transposed.  Returns (q, q_scales, qt,
+    qt_scales [C,ceil(R/128)] (groups along the rows of x; the rows of qt lie at a multiple of 16 bytes, which may be further apart than
+    R, and are written up to the next such multiple behind R, zeros from R on: torch.empty(C, -(-R//16)*16)[:, :R]).  block=True: groups of 128 x 128, scales [ceil(R/128),ceil(C/128)] and transposed.  Returns (q, q_scales, qt,
     qt_scales)."""
     lib = _lib or _library()
     if x is None or x.dim() != 2:
@@ -400,7 +400,10 @@ def sparse_fp8_quantize(x, q=None, q_scales=None, qt=None, qt_scales=None, block
         _check(qt, "qt", e4m3, (C, R))
         if qt.get_device() != device or (R > 1 and qt.stride(1) != 1):
             raise ValueError("qt must live on the device of x, with contiguous rows")
-        pt, pitch = qt.data_ptr(), qt.stride(0) if C > 1 else -(-R // 16) * 16
+        whole = -(-R // 16) * 16                  # what is written of a row
+        pt, pitch = qt.data_ptr(), qt.stride(0) if C > 1 else whole
+        if qt.untyped_storage().nbytes() - qt.storage_offset() < (C - 1) * pitch + whole:
+            raise ValueError(f"the memory of qt must hold {whole} bytes behind the start of each row, its last one too")
     pts = _tensor(qt_scales, "qt_scales", u8, (gc if block else C, gr), device, qt is None)
     rc = lib.sparse_fp8_quantize(px, pq, ps, pt, pts, pitch, R, C, int(bool(block)), _stream_ptr(stream))
     if rc != 0:
