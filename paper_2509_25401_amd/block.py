@@ -256,6 +256,8 @@ def sparse_block_norm_backward(dh, dx_out, x_out, y, dx, dy=None, norm="layer", 
 
 def sparse_rotary_frequencies(axes, theta=10000.0):
     """[theta^(-2i/d) for each axis of d channels and its d/2 pairs i] as the library computes them."""
+    if any(d < 0 for d in axes):
+        raise ValueError(f"axes must not be negative, got {tuple(axes)}")
     n = sum(int(d) // 2 for d in axes)
     buf = (ctypes.c_double * max(n, 1))()
     (_lib or _library()).sparse_rotary_frequencies(len(axes), (_i32 * len(axes))(*axes), float(theta), buf)

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <initializer_list>
 
 #include "sparse_attn.h"
@@ -680,7 +681,7 @@ int sparse_block_norm(const sparse_block_norm_args* a, void* hip_stream) {
   if (!a->x || (a->y && !a->x_out) || (!a->y && !a->h)) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: x, x_out (with y) and h or y must not be NULL", who);
   if (!a->y && (a->post_weight || a->gate)) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: gate and post_weight need y", who);
   if (f8 != (a->h_scales != nullptr)) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: h_scales goes with an E4M3 h", who);
-  const long long vectors = (a->rows + a->rows_per_vector - 1) / a->rows_per_vector;
+  const long long vectors = (a->rows - 1) / a->rows_per_vector + 1;
   if (a->scale_stride < 0 || a->shift_stride < 0 || a->gate_stride < 0) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: strides must not be negative", who);
   const size_t n = (size_t)a->rows * a->channels, xs = type_size(a->x_dtype), vs = type_size(a->vector_dtype);
   auto vec_bytes = [&](long long stride) { return ((size_t)(vectors - 1) * stride + a->channels) * vs; };
@@ -717,7 +718,7 @@ int sparse_block_norm_backward(const sparse_block_norm_backward_args* a, void* h
     return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: a weight's gradient needs the weight", who);
   if (a->scale_stride < 0 || a->gate_stride < 0) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: strides must not be negative", who);
   const int C = a->channels;
-  const long long vectors = (a->rows + a->rows_per_vector - 1) / a->rows_per_vector;
+  const long long vectors = (a->rows - 1) / a->rows_per_vector + 1;
   const size_t n = (size_t)a->rows * C, xs = type_size(a->x_dtype), vs = type_size(a->vector_dtype);
   auto vec_bytes = [&](long long stride) { return ((size_t)(vectors - 1) * stride + C) * vs; };
   const size_t sums = (size_t)vectors * C * 4;
@@ -737,7 +738,7 @@ int sparse_block_norm_backward(const sparse_block_norm_backward_args* a, void* h
   // Chunks of a vector's rows: their teams run in rounds of as many as fit the chip, and each has about six rows' worth of
   // work of its own (vectors to read, sums to write and to add up): the number with the shortest rounds.  33024 x 3072 in 129
   // vectors 275 us; with chunks for one round of all slots, whatever is left over, 408, and without the six rows 1263.
-  const long long rpv = min(a->rows_per_vector, a->rows);
+  const long long rpv = std::min(a->rows_per_vector, a->rows);
   const long long slots = 256 * teams_of(row_waves(C));
   long long chunks = 1, per = rpv, best = 1LL << 62;
   for (long long n = 1; n <= 1024 && n <= rpv; ++n) {
@@ -765,7 +766,7 @@ int sparse_block_norm_backward(const sparse_block_norm_backward_args* a, void* h
   float* we = !a->dpost_weight ? nullptr : vectors > 1 ? part + 3 * plane + extra : a->dpost_weight;
   FinishParams f = {part, part + 3 * plane + 2 * extra, a->weight, a->scale, a->gate, a->post_weight, a->dscale, a->dshift, a->dgate, wa, we, vectors,
                     a->scale_stride, a->gate_stride, C, (int)chunks};
-  const unsigned blocks = (unsigned)((C + 255) / 256), y = (unsigned)min(vectors, 65535LL);
+  const unsigned blocks = (unsigned)((C + 255) / 256), y = (unsigned)std::min(vectors, 65535LL);
   if (runs) {
     hipLaunchKernelGGL(block_norm_fold_kernel, dim3(blocks, y, (unsigned)runs), dim3(256), 0, stream, f);
     f.part = f.folded;

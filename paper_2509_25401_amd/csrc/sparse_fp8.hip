@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <utility>
 
@@ -901,14 +902,14 @@ Route route_of(long long M, long long N, int groups) {
     const long long tiles = ceil_div(M, c.m) * ceil_div(N, c.n);
     if (tiles > 0x3fffffff) continue;
     // the reduction is split where it is long and the tiles are few: joining costs a launch and the sums' traffic
-    const long long most = tiles < 256 ? min(512 / tiles, (long long)groups / 16) : 1;
-    for (long long splits = 1; splits <= max(1LL, most); splits *= 2) {
+    const long long most = tiles < 256 ? std::min(512 / tiles, (long long)groups / 16) : 1;
+    for (long long splits = 1; splits <= std::max(1LL, most); splits *= 2) {
       Route r = {0, t, 1, (int)ceil_div(groups, splits), 0};
       r.splits = (int)ceil_div(groups, r.per_split);
       r.scratch = r.splits > 1 ? (size_t)r.splits * M * N * 4 : 0;
       const long long per_cu = ceil_div(tiles * r.splits, 256);
       // sums are written and read at 4 TB/s
-      long long cost = 200 + max(3LL, c.rate * per_cu - c.less) * (r.per_split * (long long)c.stage + 200) / 3;
+      long long cost = 200 + std::max(3LL, c.rate * per_cu - c.less) * (r.per_split * (long long)c.stage + 200) / 3;
       if (r.splits > 1) cost += 400 + (long long)r.splits * M * N * 8 / 40000;
       consider(r, cost);
     }

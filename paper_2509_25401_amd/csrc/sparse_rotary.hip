@@ -23,6 +23,7 @@ namespace {
 using namespace sa_block;
 
 constexpr int kMaxAxes = 4, kMaxPairs = 128;
+constexpr int kMaxHeads = 1 << 20;     // so that their channels are counted in 32 bits
 
 struct RotaryParams {
   const __bf16* qkv;
@@ -357,9 +358,11 @@ bool rows_clash(const View& a, const View& b, int B, int L, int D) {
 
 int check_rotary(const char* who, const sparse_rotary_args* a, RotaryParams& p) {
   if (!a) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: args must not be NULL", who);
-  if (a->B <= 0 || a->L <= 0 || a->heads_q < 0 || a->heads_kv < 0 || a->heads_q + a->heads_kv <= 0)
+  if (a->B <= 0 || a->L <= 0 || a->heads_q < 0 || a->heads_kv < 0 || (a->heads_q == 0 && a->heads_kv == 0))
     return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: B=%d, L=%d must be positive, heads_q=%d and heads_kv=%d not negative nor both 0", who, a->B, a->L,
                    a->heads_q, a->heads_kv);
+  if (a->heads_q > kMaxHeads || a->heads_kv > kMaxHeads)
+    return sa_fail(SPARSE_ATTN_ERR_UNSUPPORTED, "%s: at most %d heads of a kind, got %d and %d", who, kMaxHeads, a->heads_q, a->heads_kv);
   if (a->D != 32 && a->D != 64 && a->D != 128 && a->D != 256) return sa_fail(SPARSE_ATTN_ERR_UNSUPPORTED, "%s: D=%d must be 32, 64, 128 or 256", who, a->D);
   if (a->axes < 1 || a->axes > kMaxAxes) return sa_fail(SPARSE_ATTN_ERR_UNSUPPORTED, "%s: axes=%d must be between 1 and %d", who, a->axes, kMaxAxes);
   if (!a->positions || !a->axis_channels) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: positions and axis_channels must not be NULL", who);

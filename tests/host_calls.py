@@ -154,5 +154,14 @@ def rotary_views(cases):
     return out
 
 
+def calls(cases):
+    """[method, arguments, keywords] each: [return value, message, record]"""
+    lib, out = Library(), []
+    for kind, args, kw in cases:
+        rc = getattr(lib, kind)(*args, **kw)
+        out.append([rc, lib.error() if rc else "", [e[1:] for e in lib.take()]])
+    return out
+
+
 if __name__ == "__main__":
     print(json.dumps(globals()[sys.argv[1]](*json.loads(sys.argv[2]))))
