@@ -263,10 +263,9 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) block_norm_kernel(const Norm
 struct BackParams {
   const void *dh, *dx_out, *x, *y, *weight, *scale, *gate, *post_weight;
   void *dx, *dy;
-  float* part;            // [3][vectors * chunks][C]: S, A, E
+  float* part[3];         // S, A, E, each [vectors * chunks][C], or NULL where nobody asks for it
   long long rows, rows_per_vector, vectors, scale_stride, gate_stride;
   int C, layer, chunks, rows_per_chunk, row_waves;
-  int want_s, want_a, want_e;
   float alpha, eps, post_eps;
 };
 
@@ -452,8 +451,6 @@ __global__ void __launch_bounds__(THREADS) block_norm_backward_kernel(const Back
     for (int k = 0; k < kAhead; ++k)
       if (i + k < p.rows_per_chunk) process(buffer[k], first + i + k);
   if (chunk >= all) return;
-  const size_t plane = (size_t)all * p.C;
-  float* part = p.part + (size_t)chunk * p.C;
   auto store = [&](float* to, const float (&v)[NV][8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < NV; ++u)
@@ -466,17 +463,18 @@ __global__ void __launch_bounds__(THREADS) block_norm_backward_kernel(const Back
           if (at.has(u, e)) to[at.channel(u, e)] = v[u][e];
       }
   };
-  if (p.want_s) store(part, S);
-  if (p.want_a) store(part + plane, A);
-  if (p.want_e) store(part + 2 * plane, E);
+  const size_t own = (size_t)chunk * p.C;
+  if (p.part[0]) store(p.part[0] + own, S);
+  if (p.part[1]) store(p.part[1] + own, A);
+  if (p.part[2]) store(p.part[2] + own, E);
 }
 
 // Sums of the chunks of a vector, a column to a thread, in their order but kAtOnce strands at a time so that the loads overlap.
 // Where there are more than kFold of them, a first pass folds runs of kFold into one: 5 us for 512 chunks of 3072 channels, and
 // 5 for the rest; one pass over all of them 40 us.
 struct FinishParams {
-  const float* part;      // [3][vectors * chunks][C]
-  float* folded;          // [3][vectors * runs][C]
+  const float* part[3];   // S, A, E, each [vectors * chunks][C]; what nobody asks for is one of the others
+  float* folded[3];       // each [vectors * runs][C], or NULL
   const void *weight, *scale, *gate, *post_weight;
   float *dscale, *dshift, *dgate;
   float *wa, *we;         // [vectors][C]: what dweight and dpost_weight are the sums of (the results themselves with one vector), or NULL
@@ -486,10 +484,10 @@ struct FinishParams {
 
 constexpr int kFold = 32;
 
-// n >= 1 rows of `pitch` floats in N planes that are `plane` apart.  Loads are not put under conditions, which would make each
-// wait for the one before: rows past the end repeat the last one, planes that nobody asked for hold anything and are not used.
+// Sums of n >= 1 rows of `pitch` floats, from column `at` of N planes.  Loads are not put under conditions, which would make each
+// wait for the one before: rows past the end repeat the last one.
 template <int N>
-__device__ __forceinline__ void column_sums(const float* p, size_t plane, long long n, size_t pitch, float (&out)[N]) {
+__device__ __forceinline__ void column_sums(const float* const (&p)[N], size_t at, long long n, size_t pitch, float (&out)[N]) {
   constexpr int kAtOnce = 8;
   float s[kAtOnce][N] = {};
   for (long long i = 0; i < n; i += kAtOnce) {
@@ -497,7 +495,7 @@ __device__ __forceinline__ void column_sums(const float* p, size_t plane, long l
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k)
 #pragma unroll
-      for (int a = 0; a < N; ++a) v[k][a] = p[min(i + k, n - 1) * pitch + a * plane];
+      for (int a = 0; a < N; ++a) v[k][a] = p[a][at + min(i + k, n - 1) * pitch];
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k)
 #pragma unroll
@@ -512,9 +510,10 @@ __global__ void __launch_bounds__(256) block_norm_fold_kernel(const FinishParams
   if (c >= p.C) return;
   for (long long g = blockIdx.y; g < p.vectors; g += gridDim.y) {
     float s[3];
-    column_sums(p.part + ((size_t)g * p.chunks + run * kFold) * p.C + c, (size_t)p.vectors * p.chunks * p.C, min(kFold, p.chunks - run * kFold), p.C, s);
+    column_sums(p.part, ((size_t)g * p.chunks + run * kFold) * p.C + c, min(kFold, p.chunks - run * kFold), p.C, s);
 #pragma unroll
-    for (int a = 0; a < 3; ++a) p.folded[((size_t)a * p.vectors * runs + (size_t)g * runs + run) * p.C + c] = s[a];
+    for (int a = 0; a < 3; ++a)
+      if (p.folded[a]) p.folded[a][((size_t)g * runs + run) * p.C + c] = s[a];
   }
 }
 
@@ -524,23 +523,25 @@ __global__ void __launch_bounds__(256) block_norm_finish_kernel(const FinishPara
   if (c >= p.C) return;
   for (long long g = blockIdx.y; g < p.vectors; g += gridDim.y) {
     float s[3];
-    column_sums(p.part + (size_t)g * p.chunks * p.C + c, (size_t)p.vectors * p.chunks * p.C, p.chunks, p.C, s);
+    column_sums(p.part, (size_t)g * p.chunks * p.C + c, p.chunks, p.C, s);
     const long long at = g * p.C + c;
-    if (p.dshift) p.dshift[at] = s[0];
-    if (p.dscale) p.dscale[at] = p.weight ? s[1] * (float)((const TV*)p.weight)[c] : s[1];
+    // with one chunk to a vector these may be the results' own places, where they stay if no factor follows
+    if (p.dshift && p.dshift != p.part[0]) p.dshift[at] = s[0];
+    if (p.dscale && (p.weight || p.dscale != p.part[1])) p.dscale[at] = p.weight ? s[1] * (float)((const TV*)p.weight)[c] : s[1];
     if (p.wa) p.wa[at] = p.scale ? s[1] * (1.f + (float)((const TV*)p.scale)[g * p.scale_stride + c]) : s[1];
-    if (p.dgate) p.dgate[at] = p.post_weight ? s[2] * (float)((const TV*)p.post_weight)[c] : s[2];
+    if (p.dgate && (p.post_weight || p.dgate != p.part[2])) p.dgate[at] = p.post_weight ? s[2] * (float)((const TV*)p.post_weight)[c] : s[2];
     if (p.we) p.we[at] = p.gate ? s[2] * (float)((const TV*)p.gate)[g * p.gate_stride + c] : s[2];
   }
 }
 
-// [2][n][C]: what the two weights' gradients are the sums of; 64 columns and sixteen shares of the vectors to a workgroup
-__global__ void __launch_bounds__(1024) column_sum_kernel(const float* part, float* dweight, float* dpost, long long n, int C) {
+// wa, we [n][C]: what the two weights' gradients are the sums of; 64 columns and sixteen shares of the vectors to a workgroup
+__global__ void __launch_bounds__(1024) column_sum_kernel(const float* wa, const float* we, float* dweight, float* dpost, long long n, int C) {
   __shared__ float red[16][2][64];
   const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   const long long per = (n + 15) / 16, first = share * per, count = min(per, n - first);
   float s[2] = {0.f, 0.f};
-  if (c < C && count > 0) column_sums(part + first * C + c, (size_t)n * C, count, C, s);
+  const float* const part[2] = {wa, we};
+  if (c < C && count > 0) column_sums(part, first * C + c, count, C, s);
   red[share][0][lane] = s[0];
   red[share][1][lane] = s[1];
   __syncthreads();
@@ -659,6 +660,23 @@ void launch_backward(BackParams& p, bool vec, hipStream_t stream) {
   else vec ? go(N1{}, T{}, Twelve{}) : go(N1{}, F{}, Twelve{});
 }
 
+// Chunks of a vector's rows: their teams run in rounds of as many as fit the chip, and each has about six rows' worth of
+// work of its own (vectors to read, sums to write and to add up): the number with the shortest rounds.  33024 x 3072 in 129
+// vectors 275 us; with chunks for one round of all slots, whatever is left over, 408, and without the six rows 1263.
+struct ChunkPlan {
+  int chunks, rows;
+};
+ChunkPlan chunks_of(long long rpv, long long vectors, int C) {
+  const long long slots = 256 * teams_of(row_waves(C));
+  long long best = 1LL << 62;
+  ChunkPlan plan = {1, (int)rpv};
+  for (long long n = 1; n <= 1024 && n <= rpv; ++n) {
+    const long long per = (rpv + n - 1) / n, cost = (vectors * n + slots - 1) / slots * (per + 6);
+    if (cost < best) best = cost, plan = {(int)((rpv + per - 1) / per), (int)per};
+  }
+  return plan;
+}
+
 template <class F>
 void by_types(int x_dtype, int vector_dtype, F&& f) {
   if (x_dtype == SPARSE_BLOCK_F32)
@@ -735,41 +753,52 @@ int sparse_block_norm_backward(const sparse_block_norm_backward_args* a, void* h
   const bool vec = C % 8 == 0 && aligned16(a->dh) && aligned16(a->dx_out) && aligned16(a->x_out) && aligned16(a->y) && aligned16(a->dx) &&
                    aligned16(a->dy) && aligned16(a->weight) && aligned16(a->scale) && aligned16(a->gate) && aligned16(a->post_weight) &&
                    (a->scale_stride | a->gate_stride) % 8 == 0;
-  // Chunks of a vector's rows: their teams run in rounds of as many as fit the chip, and each has about six rows' worth of
-  // work of its own (vectors to read, sums to write and to add up): the number with the shortest rounds.  33024 x 3072 in 129
-  // vectors 275 us; with chunks for one round of all slots, whatever is left over, 408, and without the six rows 1263.
-  const long long rpv = std::min(a->rows_per_vector, a->rows);
-  const long long slots = 256 * teams_of(row_waves(C));
-  long long chunks = 1, per = rpv, best = 1LL << 62;
-  for (long long n = 1; n <= 1024 && n <= rpv; ++n) {
-    const long long rows = (rpv + n - 1) / n, cost = (vectors * n + slots - 1) / slots * (rows + 6);
-    if (cost < best) best = cost, chunks = (rpv + rows - 1) / rows, per = rows;
-  }
-  if (vectors * chunks > 0x7fffffffLL) return sa_fail(SPARSE_ATTN_ERR_UNSUPPORTED, "%s: too many modulation vectors", who);
   hipStream_t stream = (hipStream_t)hip_stream;
-  const bool want_s = a->dshift, want_a = a->dscale || a->dweight, want_e = a->dgate || a->dpost_weight;
-  const size_t plane = (size_t)vectors * chunks * C;
-  const size_t extra = vectors > 1 ? (size_t)vectors * C : 0;
-  const int runs = chunks > kFold ? (int)((chunks + kFold - 1) / kFold) : 0;
-  const size_t folded = (size_t)vectors * runs * C;
+  const ChunkPlan plan = chunks_of(std::min(a->rows_per_vector, a->rows), vectors, C);
+  if (vectors * plan.chunks > 0x7fffffffLL) return sa_fail(SPARSE_ATTN_ERR_UNSUPPORTED, "%s: too many modulation vectors", who);
+  const size_t VC = (size_t)vectors * C, plane = VC * plan.chunks;
+  const int runs = plan.chunks > kFold ? (plan.chunks + kFold - 1) / kFold : 0;
+  const bool want[3] = {a->dshift != nullptr, a->dscale || a->dweight, a->dgate || a->dpost_weight};
+  float* const result[3] = {a->dshift, a->dscale, a->dgate};
+  // Scratch memory: the chunks' sums, then those of the runs.  With one chunk to a vector they are the results up to a factor
+  // and are kept there.  What the weights' gradients are the sums of: their own places with one vector.
+  size_t need = 0, planes = 0;
+  auto take = [&](bool wanted, size_t floats) {
+    const size_t at = need;
+    if (wanted) need += floats;
+    return at;
+  };
+  size_t at_part[3], at_folded[3];
+  for (int i = 0; i < 3; ++i) {
+    planes += want[i];
+    at_part[i] = take(want[i] && (plan.chunks > 1 || !result[i]), plane);
+    at_folded[i] = take(want[i] && runs, VC * runs);
+  }
+  const size_t at_wa = take(a->dweight && vectors > 1, VC), at_we = take(a->dpost_weight && vectors > 1, VC);
   sa_scratch scratch;
-  if (want_s || want_a || want_e)
-    if (int rc = scratch.get((3 * plane + 2 * extra + 3 * folded) * 4, stream)) return rc;
-  float* part = (float*)scratch.data();
-  BackParams p = {a->dh, a->dx_out, a->x_out, a->y, a->weight, a->scale, a->gate, a->post_weight, a->dx, a->dy, part, a->rows,
-                  a->rows_per_vector, vectors, a->scale_stride, a->gate_stride, C, a->norm == SPARSE_BLOCK_NORM_LAYER, (int)chunks, (int)per, 0,
-                  want_s, want_a, want_e, a->y ? a->alpha : 1.f, a->eps, a->post_eps};
+  if (need)
+    if (int rc = scratch.get(need * 4, stream)) return rc;
+  float* const base = (float*)scratch.data();
+  BackParams p = {a->dh, a->dx_out, a->x_out, a->y, a->weight, a->scale, a->gate, a->post_weight, a->dx, a->dy, {}, a->rows,
+                  a->rows_per_vector, vectors, a->scale_stride, a->gate_stride, C, a->norm == SPARSE_BLOCK_NORM_LAYER, plan.chunks, plan.rows, 0,
+                  a->y ? a->alpha : 1.f, a->eps, a->post_eps};
+  for (int i = 0; i < 3; ++i) p.part[i] = !want[i] ? nullptr : plan.chunks == 1 && result[i] ? result[i] : base + at_part[i];
   by_types(a->x_dtype, a->vector_dtype, [&](auto tx, auto tv) { launch_backward<decltype(tx), decltype(tv)>(p, vec, stream); });
   if (int rc = launched(who)) return rc;
-  if (!part) return 0;
-  float* wa = !a->dweight ? nullptr : vectors > 1 ? part + 3 * plane : a->dweight;
-  float* we = !a->dpost_weight ? nullptr : vectors > 1 ? part + 3 * plane + extra : a->dpost_weight;
-  FinishParams f = {part, part + 3 * plane + 2 * extra, a->weight, a->scale, a->gate, a->post_weight, a->dscale, a->dshift, a->dgate, wa, we, vectors,
-                    a->scale_stride, a->gate_stride, C, (int)chunks};
+  if (!planes) return 0;
+  float* wa = !a->dweight ? nullptr : vectors > 1 ? base + at_wa : a->dweight;
+  float* we = !a->dpost_weight ? nullptr : vectors > 1 ? base + at_we : a->dpost_weight;
+  FinishParams f = {{}, {}, a->weight, a->scale, a->gate, a->post_weight, a->dscale, a->dshift, a->dgate, wa, we, vectors,
+                    a->scale_stride, a->gate_stride, C, plan.chunks};
+  const int some = want[0] ? 0 : want[1] ? 1 : 2;
+  for (int i = 0; i < 3; ++i) {
+    f.part[i] = p.part[want[i] ? i : some];
+    f.folded[i] = want[i] && runs ? base + at_folded[i] : nullptr;
+  }
   const unsigned blocks = (unsigned)((C + 255) / 256), y = (unsigned)std::min(vectors, 65535LL);
   if (runs) {
     hipLaunchKernelGGL(block_norm_fold_kernel, dim3(blocks, y, (unsigned)runs), dim3(256), 0, stream, f);
-    f.part = f.folded;
+    for (int i = 0; i < 3; ++i) f.part[i] = f.folded[want[i] ? i : some];
     f.chunks = runs;
   }
   if (a->vector_dtype == SPARSE_BLOCK_F32)
@@ -778,7 +807,7 @@ int sparse_block_norm_backward(const sparse_block_norm_backward_args* a, void* h
     hipLaunchKernelGGL(block_norm_finish_kernel<__bf16>, dim3(blocks, y), dim3(256), 0, stream, f);
   const unsigned columns = (unsigned)((C + 63) / 64);
   if (vectors > 1 && (wa || we))
-    hipLaunchKernelGGL(column_sum_kernel, dim3(columns), dim3(1024), 0, stream, part + 3 * plane, a->dweight, a->dpost_weight, vectors, C);
+    hipLaunchKernelGGL(column_sum_kernel, dim3(columns), dim3(1024), 0, stream, wa ? wa : we, we ? we : wa, a->dweight, a->dpost_weight, vectors, C);
   return launched(who);
 }
 
