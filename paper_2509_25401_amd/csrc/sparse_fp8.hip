@@ -869,7 +869,6 @@ struct Route {
   int ki;                      // large kernel: rows of a tile / 32; 0: the kernel for the others, with
   int tile;                    // one of kTiles, and
   int splits, per_split;       // parts of the reduction, groups in each
-  size_t scratch;
 };
 
 // rows, columns, what a stage costs a CU (us / 100), and how many thirds of a workgroup's time n of them take on one CU:
@@ -878,6 +877,19 @@ struct TileCost {
   int m, n, stage, rate, less;
 };
 constexpr TileCost kTiles[] = {{128, 128, 64, 3, 0}, {64, 64, 27, 2, 0}, {32, 64, 24, 3, 1}};
+
+constexpr long long kMostSplitTiles = 512;     // tiles times splits, at most
+constexpr int kLeastSplit = 16;                // groups of a split, about
+
+// Scratch memory that a product of these sizes may take, whichever its route: the splits' sums or the packed scales.  It does not
+// grow when a size shrinks, unlike what the routes need (of 3072 columns and 12288 channels: one row 48 KiB, in four splits, 400
+// rows nothing), so that no later and smaller call finds too little: such a call may be under capture.
+size_t scratch_of(long long M, long long N, int groups) {
+  size_t sums = 0, scales = 0;
+  if (groups >= 2 * kLeastSplit) sums = (size_t)std::min(groups / kLeastSplit * M * N, kMostSplitTiles * kTiles[0].m * kTiles[0].n) * 4;
+  if (M >= 128 && groups >= 3) scales = (size_t)(ceil_div(M, 128) + ceil_div(N, kBig)) * 2 * ((groups + 1) & ~1) * 128;
+  return sums > scales ? sums : scales;
+}
 
 // Takes the route that a small model of the times calls the fastest.  Its constants are measured (us / 100), over 1 to 33024
 // rows, 300 to 18432 columns and 128 to 9008 channels; what it is right to within (15 %) is less than what the routes differ by
@@ -902,11 +914,10 @@ Route route_of(long long M, long long N, int groups) {
     const long long tiles = ceil_div(M, c.m) * ceil_div(N, c.n);
     if (tiles > 0x3fffffff) continue;
     // the reduction is split where it is long and the tiles are few: joining costs a launch and the sums' traffic
-    const long long most = tiles < 256 ? std::min(512 / tiles, (long long)groups / 16) : 1;
+    const long long most = tiles < 256 ? std::min(kMostSplitTiles / tiles, (long long)groups / kLeastSplit) : 1;
     for (long long splits = 1; splits <= std::max(1LL, most); splits *= 2) {
-      Route r = {0, t, 1, (int)ceil_div(groups, splits), 0};
+      Route r = {0, t, 1, (int)ceil_div(groups, splits)};
       r.splits = (int)ceil_div(groups, r.per_split);
-      r.scratch = r.splits > 1 ? (size_t)r.splits * M * N * 4 : 0;
       const long long per_cu = ceil_div(tiles * r.splits, 256);
       // sums are written and read at 4 TB/s
       long long cost = 200 + std::max(3LL, c.rate * per_cu - c.less) * (r.per_split * (long long)c.stage + 200) / 3;
@@ -921,9 +932,8 @@ Route route_of(long long M, long long N, int groups) {
     const long long tiles_m = ceil_div(M, 32 * ki), tiles = tiles_m * ceil_div(N, kBig);
     if (tiles > 0x3fffffff) continue;
     const int stages = (groups + 1) & ~1;
-    Route r = {ki, 0, 1, 0, (size_t)(tiles_m + ceil_div(N, kBig)) * 2 * stages * 128};
     const long long rounds = ceil_div(ceil_div(tiles, 8), 32);
-    consider(r, 600 + rounds * ((long long)stages * stage[ki - 4] + 350));
+    consider({ki, 0, 1, 0}, 600 + rounds * ((long long)stages * stage[ki - 4] + 350));
   }
   return best;
 }
@@ -962,7 +972,7 @@ int launch_split(const char* who, const GemmParams& p, const Route& r, float* pa
   return launched(who);
 }
 
-// scratch: r.scratch bytes, 256-byte aligned
+// scratch: scratch_of() bytes, 256-byte aligned
 int launch_gemm(const char* who, const GemmParams& p, const Route& r, uint8_t* scratch, hipStream_t stream) {
   if (r.ki == 0)
     switch (r.tile) {
@@ -1055,8 +1065,8 @@ int sparse_fp8_gemm(const void* a, const uint8_t* a_scales, int a_block, const v
                         a_block ? 7 : 0, b_block ? 7 : 0, size == 4};
   const Route r = route_of(M, N, groups);
   sa_scratch scratch;
-  if (r.scratch)
-    if (int rc = scratch.get(r.scratch, (hipStream_t)hip_stream)) return rc;
+  if (const size_t need = scratch_of(M, N, groups))
+    if (int rc = scratch.get(need, (hipStream_t)hip_stream)) return rc;
   return launch_gemm(who, p, r, (uint8_t*)scratch.data(), (hipStream_t)hip_stream);
 }
 
@@ -1077,7 +1087,7 @@ int sparse_fp8_linear(const void* x, const void* w, const uint8_t* w_scales, con
   sa_scratch scratch;
   const Route r = route_of(M, N, groups);
   const size_t held = rounded((size_t)M * K), scaled = rounded((size_t)M * groups);
-  if (int rc = scratch.get(held + scaled + r.scratch, stream)) return rc;
+  if (int rc = scratch.get(held + scaled + scratch_of(M, N, groups), stream)) return rc;
   uint8_t *x8 = (uint8_t*)scratch.data(), *xs = x8 + held;
   launch_quantize({(const __bf16*)x, x8, xs, nullptr, nullptr, nullptr, M, K, 0}, false, stream);
   const GemmParams p = {x8, xs, (const uint8_t*)w, w_scales, (const __bf16*)bias, out, M, N, K, K, (int)K, groups, 0, 7, size == 4};
@@ -1115,7 +1125,7 @@ int sparse_fp8_linear_backward(const void* dy, const void* x, const void* wt, co
   };
   const size_t at_dy = take(dx, (size_t)M * N), at_dys = take(dx, (size_t)M * groups_n), at_dyt = take(dw, (size_t)N * pitch),
                at_dyts = take(dw, (size_t)N * groups_m), at_xt = take(dw, (size_t)K * pitch), at_xts = take(dw, (size_t)K * groups_m),
-               at_part = take(dbias, (size_t)groups_m * N * 4), at_x = take(dx, rx.scratch), at_w = take(dw, rw.scratch);
+               at_part = take(dbias, (size_t)groups_m * N * 4), at_x = take(dx, scratch_of(M, K, groups_n)), at_w = take(dw, scratch_of(N, K, groups_m));
   sa_scratch scratch;
   if (int rc = scratch.get(need, stream)) return rc;
   uint8_t* base = (uint8_t*)scratch.data();

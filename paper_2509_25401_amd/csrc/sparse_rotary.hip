@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "sparse_attn.h"
@@ -411,8 +412,9 @@ int check_rotary(const char* who, const sparse_rotary_args* a, RotaryParams& p) 
 // Few tokens: their heads are dealt to several workgroups, so that the call fills the chip and a wave's walk is short.  72 heads
 // of 128, forward, against one workgroup for all heads: 64 tokens 4.6 us / 21, 512 tokens 7 / 23, 4608 tokens 36 / 47, from some
 // 8192 tokens on the same.
+constexpr int kFewParts = 512;
 int head_parts(long long groups, int heads) {
-  long long parts = (512 + groups - 1) / groups;
+  long long parts = (kFewParts + groups - 1) / groups;
   return (int)(parts < 1 ? 1 : parts > heads ? heads : parts);
 }
 
@@ -506,7 +508,9 @@ int sparse_rotary_heads_backward(const sparse_rotary_args* a, void* dqkv, long l
   const size_t n = (size_t)grid.x * grid.y;
   sa_scratch scratch;
   if (sums) {
-    if (int rc = scratch.get(n * 2 * a->D * 4, stream)) return rc;
+    // as many as there are workgroups with these sizes or smaller ones: a smaller call has then what it needs
+    const long long most_n = std::min(groups * heads, groups + kFewParts - 1);
+    if (int rc = scratch.get(most_n * 2 * a->D * 4, stream)) return rc;
     p.part = (float*)scratch.data();
   }
   by_shape(a->D, p.halves, [&](auto d, auto h) {

@@ -108,6 +108,9 @@ class Library:
         width = (Hq + 2 * Hkv) * D
         return self.lib.sparse_rotary_heads_backward(ctypes.byref(self.rotary_args(B, L, Hq, Hkv, D)), at(7), L * width, width, at(8), at(9), None)
 
+    def release(self):
+        return self.lib.sparse_attn_release_scratch(None)
+
     def attention(self, B, H, L, D):
         return self.lib.sparse_attn_fwd(at(0), at(1), at(2), at(3), at(4), None, at(5), B, H, L, D, 128, 128)
 
