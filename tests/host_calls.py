@@ -24,7 +24,7 @@ def run(scenario, *args, _built=[]):
         subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wl,-soname,libamdhip64.so.7", "-Wl,--version-script=" + versions,
                                "-o", os.path.join(at, "libamdhip64.so.7"), os.path.join(HERE, "fake_hip.cpp")])
     env = dict(os.environ, LD_LIBRARY_PATH=_built[0].name, PYTHONPATH=ROOT)
-    out = subprocess.run([sys.executable, os.path.abspath(__file__), scenario, json.dumps(args)], env=env, stdout=subprocess.PIPE, timeout=120, check=True)
+    out = subprocess.run([sys.executable, os.path.abspath(__file__), scenario], input=json.dumps(args).encode(), env=env, stdout=subprocess.PIPE, timeout=120, check=True)
     return json.loads(out.stdout)
 
 
@@ -167,4 +167,4 @@ def calls(cases):
 
 
 if __name__ == "__main__":
-    print(json.dumps(globals()[sys.argv[1]](*json.loads(sys.argv[2]))))
+    print(json.dumps(globals()[sys.argv[1]](*json.load(sys.stdin))))
