@@ -16,18 +16,22 @@ using namespace sa_block;
 
 constexpr int kMaxChannels = 16384;
 
-// Where the values of a row lie among the threads that share it: unit u of thread t is eight consecutive channels.  VEC: rows
-// are whole units on 16 bytes; else they start at any element, and the last unit of a row may have fewer channels.
-template <bool VEC>
+// How the rows lie: whole units on 16 bytes; or from any element on, where the last unit of a row may have fewer channels.  Its
+// thread then either reads the row's last eight channels and moves those that are its own to their places, so that no load stands
+// under a condition and waits for the one before; or reads its channels one by one, the others' runs standing under the condition.
+enum Rows { kWhole, kTailMoved, kTailApart };
+
+// Where the values of a row lie among the threads that share it: unit u of thread t is eight consecutive channels.
+template <Rows ROWS>
 struct Place {
   int t, threads, C;
   __device__ __forceinline__ int channel(int u, int e) const { return (u * threads + t) * 8 + e; }
-  __device__ __forceinline__ bool has(int u, int e) const { return channel(u, VEC ? 0 : e) < C; }
+  __device__ __forceinline__ bool has(int u, int e) const { return channel(u, ROWS == kWhole ? 0 : e) < C; }
   // Behind Unit::load(), before the first use: values of channels that do not exist become zeros.  The last unit of a row holds the
   // row's last eight channels until then, and moves down those that are its own.
   template <class... F>
   __device__ __forceinline__ void settle(int u, F&... f) const {
-    if constexpr (!VEC) {
+    if constexpr (ROWS == kTailMoved) {
       if (has(u, 7)) return;
       const int away = has(u, 0) && C >= 8 ? 8 - (C & 7) : 0;
 #pragma unroll
@@ -43,7 +47,7 @@ struct Place {
   }
 };
 
-template <class T, bool VEC>
+template <class T, Rows ROWS>
 struct Unit {
   Pack8<T> v;
   __device__ __forceinline__ void zero() {
@@ -51,22 +55,34 @@ struct Unit {
     for (int e = 0; e < 8; ++e) v.set(e, 0.f);
   }
   template <bool ONCE>
-  __device__ __forceinline__ void load(const T* row, const Place<VEC>& p, int u) {
-    if constexpr (VEC) {
+  __device__ __forceinline__ void load(const T* row, const Place<ROWS>& p, int u) {
+    if constexpr (ROWS == kWhole) {
       if (!p.has(u, 0)) return zero();
       if (ONCE)
         v.load_once(row + p.channel(u, 0));
       else
         v.load(row + p.channel(u, 0));
+    } else if constexpr (ROWS == kTailApart) {
+      if (p.has(u, 7)) {
+        v.load_any(row + p.channel(u, 0));
+      } else if (p.has(u, 0)) {
+        T one[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) one[e] = row[min(p.channel(u, e), p.C - 1)];     // all on their way together
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.set(e, p.has(u, e) ? (float)one[e] : 0.f);
+      } else {
+        zero();
+      }
     } else if (p.C >= 8) {
-      v.load_any(row + min(p.channel(u, 0), p.C - 8));       // under no condition, so that no load waits for the one before
+      v.load_any(row + min(p.channel(u, 0), p.C - 8));
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v.set(e, (float)row[min(p.channel(u, e), p.C - 1)]);
     }
   }
-  __device__ __forceinline__ void store(T* row, const Place<VEC>& p, int u) const {
-    if constexpr (VEC) {
+  __device__ __forceinline__ void store(T* row, const Place<ROWS>& p, int u) const {
+    if constexpr (ROWS == kWhole) {
       if (p.has(u, 0)) v.store_once(row + p.channel(u, 0));
     } else if (p.has(u, 7)) {
       v.store_any(row + p.channel(u, 0));          // through the cache: rows share its lines
@@ -115,31 +131,37 @@ struct NormParams {
 };
 
 // One pass per row: x (and y) are read once, stay in registers through the reductions, x' and h are written once.  Bound by the
-// memory: 33024 x 3072 bf16 with y, gate, scale and shift 156 us, 5.2 TB/s; with float32 x 226 us, 5.4 TB/s; 17 x 3072 3.7 us;
-// 9001 x 3073 71 us, 3.1 TB/s, as its rows share the cache's lines.  All sums and all values in between are float32; what is rounded are
+// memory: 33024 x 3072 bf16 with y, gate, scale and shift 150 us, 5.4 TB/s; with float32 x 223 us, 5.5 TB/s; 17 x 3072 3.7 us.
+// 9001 x 3073 69 us, 3.2 TB/s: its rows' 16-byte accesses straddle lines and its stores go through the cache; how much of it either
+// costs has not been measured.  All sums and all values in between are float32; what is rounded are
 // the results: x' to its type, and h, which is of the x' before that, to bf16 or to its e4m3 form.
 // ONE: a wave per row, four rows per workgroup, no barrier; else all waves of the workgroup share a row.
 template <class TX, class TV, int NV, bool VEC, bool ONE, bool F8>
 __global__ void __launch_bounds__(ONE ? 256 : 1024) block_norm_kernel(const NormParams p) {
+  // us, tail moved / apart.  Eight units to a thread of one wave: bf16 9001 x 3073 84.5 / 69.0, float32 11776 x 2109 122.6 / 108.5.  One
+  // unit to a thread of several waves: 9001 x 4099 108.7 / 96.8, 9001 x 7001 196 / 182, 300 x 7001 11.4 / 10.0, but 1500 x 4001 16.0 /
+  // 17.3.  Else moved: 40000 x 333 43.5 / 47.8, 30000 x 1001 54.4 / 60.6, 18002 x 2001 67.3 / 72.7 (though 18002 x 1161 61.0 / 56.4),
+  // 9001 x 9001 177 / 182 (though 9001 x 16001 315 / 301).
+  constexpr Rows ROWS = VEC ? kWhole : (ONE ? NV == 8 : NV == 1) ? kTailApart : kTailMoved;
   __shared__ float slots[2][16][1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const long long row = ONE ? (long long)blockIdx.x * 4 + wave : (long long)blockIdx.x;
   if (row >= p.rows) return;                                  // whole waves; with ONE no barrier follows
-  const Place<VEC> at{ONE ? lane : (int)threadIdx.x, ONE ? 64 : (int)blockDim.x, p.C};
+  const Place<ROWS> at{ONE ? lane : (int)threadIdx.x, ONE ? 64 : (int)blockDim.x, p.C};
   RowSum<ONE, 1> sum{slots, wave, (int)blockDim.x >> 6};
   const float inv_c = 1.f / (float)p.C;
   const long long g = row / p.rows_per_vector;
   const TX* x = (const TX*)p.x + row * p.C;
 
   float v[NV][8];
-  Unit<TX, VEC> xu[NV];
+  Unit<TX, ROWS> xu[NV];
 #pragma unroll
   for (int u = 0; u < NV; ++u) xu[u].template load<true>(x, at, u);
   if (p.y) {
     const __bf16* y = (const __bf16*)p.y + row * p.C;
     const TV* gate = p.gate ? (const TV*)p.gate + g * p.gate_stride : nullptr;
     const TV* wp = (const TV*)p.post_weight;
-    Unit<__bf16, VEC> yu[NV];
+    Unit<__bf16, ROWS> yu[NV];
 #pragma unroll
     for (int u = 0; u < NV; ++u) yu[u].template load<true>(y, at, u);
     float rp = 1.f;
@@ -159,10 +181,10 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) block_norm_kernel(const Norm
     }
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      Unit<TV, VEC> gu, wu;
+      Unit<TV, ROWS> gu, wu;
       if (gate) gu.template load<false>(gate, at, u);
       if (wp) wu.template load<false>(wp, at, u);
-      Unit<TX, VEC> o;
+      Unit<TX, ROWS> o;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float t = yu[u].get(e) * rp;
@@ -210,7 +232,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) block_norm_kernel(const Norm
   const TV* shift = p.shift ? (const TV*)p.shift + g * p.shift_stride : nullptr;
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
-    Unit<TV, VEC> wu, su, bu;
+    Unit<TV, ROWS> wu, su, bu;
     if (w) wu.template load<false>(w, at, u);
     if (scale) su.template load<false>(scale, at, u);
     if (shift) bu.template load<false>(shift, at, u);
@@ -243,7 +265,7 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) block_norm_kernel(const Norm
         if ((lane & 15) == 0) p.h_scales[row * ((p.C + 127) / 128) + c / 128] = (uint8_t)(ex + 127);
       }
     } else {
-      Unit<__bf16, VEC> o;
+      Unit<__bf16, ROWS> o;
 #pragma unroll
       for (int e = 0; e < 8; ++e) o.set(e, h[e]);
       o.store((__bf16*)p.h + row * p.C, at, u);
@@ -277,16 +299,18 @@ struct BackParams {
 //     sum (x - mean)^2 = sum_w [ sum (x - m_w)^2 + n_w d_w^2 ],   sum dn (x - mean) = sum_w [ sum dn (x - m_w) + d_w sum dn ].
 // 33024 x 3072 bf16 in 16 vectors, with y and dx_out: 253 us, 4.8 TB/s of the six tensors; 9001 x 3072 80 us, 4.1 TB/s; 512 x 3072
 // 24 us, mostly the way to the first row and the sums'.  18002 x 1160 with a post norm 75 us, 3.3 TB/s: three waves to a row, the
-// last with 17 lanes of work, and two barriers; there the vector instructions bound it.  Rows at any alignment (9001 x 3073, 140 us)
-// keep one row on its way instead of two, as the registers hold no more.  Sums and values in between are float32; dx and dy are
+// last with 17 lanes of work, and two barriers; there the vector instructions bound it.  Rows at any alignment (9001 x 3073, 98 us)
+// keep one row on its way instead of two, and even so hold 26 to 42 registers' worth in scratch memory (with the tail apart 10 to 20, and
+// 142 us); so do whole rows of more than 6144 channels, 6 to 28 (4000 x 7000 93 us, 3.6 TB/s), and far more beyond 8192.  Sums and values in between are float32; dx and dy are
 // rounded once, to their types.
 template <class TX, class TV, int NV, bool VEC, int THREADS>
 __global__ void __launch_bounds__(THREADS) block_norm_backward_kernel(const BackParams p) {
+  constexpr Rows ROWS = VEC ? kWhole : kTailMoved;
   __shared__ __attribute__((aligned(16))) float slots[2][16][4];
   __shared__ float post_slots[2][16][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = p.row_waves, l16 = lane & 15;
   const int team = wave / waves, base = team * waves;          // the team's first wave
-  const Place<VEC> at{(int)threadIdx.x - base * 64, waves * 64, p.C};
+  const Place<ROWS> at{(int)threadIdx.x - base * 64, waves * 64, p.C};
   const float inv_c = 1.f / (float)p.C;
   const long long chunk = (long long)blockIdx.x * (blockDim.x / 64 / waves) + team, all = p.vectors * p.chunks;
   const long long g = min(chunk, all - 1) / p.chunks;
@@ -297,8 +321,8 @@ __global__ void __launch_bounds__(THREADS) block_norm_backward_kernel(const Back
 
   constexpr int kAhead = VEC ? 2 : 1;          // rows on their way
   struct Row {
-    Unit<TX, VEC> x[NV], dxo[NV];
-    Unit<__bf16, VEC> dh[NV], y[NV];
+    Unit<TX, ROWS> x[NV], dxo[NV];
+    Unit<__bf16, ROWS> dh[NV], y[NV];
   } buffer[kAhead];
   auto load = [&](Row& b, long long row) __attribute__((always_inline)) {
 #pragma unroll
@@ -323,7 +347,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_backward_kernel(const Back
   float count = 0.f;
   {
     // all on their way before the first is used
-    Unit<TV, VEC> w[NV], sc[NV], ga[NV], pw[NV];
+    Unit<TV, ROWS> w[NV], sc[NV], ga[NV], pw[NV];
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       if (p.weight) w[u].template load<false>((const TV*)p.weight, at, u);
@@ -419,7 +443,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_backward_kernel(const Back
         }
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        Unit<TX, VEC> r8;
+        Unit<TX, ROWS> r8;
 #pragma unroll
         for (int e = 0; e < 8; ++e) r8.set(e, p.alpha * o[u][e]);
         r8.store((TX*)p.dx + row * p.C, at, u);
@@ -436,7 +460,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_backward_kernel(const Back
       if (row < end) {
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
-          Unit<__bf16, VEC> r8;
+          Unit<__bf16, ROWS> r8;
 #pragma unroll
           for (int e = 0; e < 8; ++e) r8.set(e, rp * (o[u][e] * gp[u][e] - yf[u][e] * mean_dmm));
           r8.store((__bf16*)p.dy + row * p.C, at, u);
