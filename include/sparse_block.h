@@ -47,7 +47,8 @@ extern "C" {
  *              NULL for zeros (scale, shift) and ones (gate)
  * x, y, x_out and h are contiguous.  None of the results may overlap another argument, but x_out may be x.
  * Supported: 1 <= channels <= 16384; with E4M3 a multiple of 16, and 16-byte aligned x, y, x_out, h and vectors (8-byte
- * aligned h).  Rows that are no multiple of 8 channels, or not 16-byte aligned, are handled value by value.
+ * aligned h).  Other tensors need the alignment of their elements alone; rows that do not start on 16
+ * bytes, or are no multiple of 8 channels, move in the same runs of eight values, and slower.
  */
 typedef struct sparse_block_norm_args {
   const void* x;

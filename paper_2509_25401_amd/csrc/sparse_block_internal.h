@@ -55,8 +55,8 @@ struct Pack8<float> {
   }
 };
 
-// Sum / largest over aligned groups of N lanes (N = 2, 4, 8, 16), in every lane of the group.  Data-parallel moves inside a
-// row of 16 lanes: no trip through LDS.
+// Sum / largest over aligned groups of N lanes (N = 4, 8, 16, 32), in every lane of the group.  Data-parallel moves inside a
+// row of 16 lanes, which make no trip through LDS; the last step of 32 lanes is a shuffle, which does.
 template <int CTRL>
 __device__ __forceinline__ float moved(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));

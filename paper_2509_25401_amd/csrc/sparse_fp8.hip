@@ -546,8 +546,10 @@ __global__ void __launch_bounds__(256) join_splits_kernel(const float* part, int
 
 // ---------------------------------------------------------------------------------------
 // Large products: tiles of 128 to 256 rows and 256 columns, four waves with a quarter each, one workgroup per CU that walks over
-// its share of the tiles.  Bound by the matrix instructions: 33024 x 9216 x 3072 752 to 846 us over several chips, 2.2 to 2.48
-// PFLOP/s (the instruction alone, from registers: 4.3), 33024 x 3072 x 3072 into float32 306 us, 2.0 PFLOP/s.
+// its share of the tiles.  33024 x 9216 x 3072 735 to 810 us over several chips, 2.3 to 2.5 PFLOP/s, 33024 x 3072 x 3072 into float32
+// 306 us, 2.0 PFLOP/s.  In the first the matrix pipes are busy 63 % of the time, at 1.74 GHz (the instruction alone, from registers:
+// 4.3 PFLOP/s), and a wave waits 37 % of its own; how much of the rest is the clock under this load and how much the waits has not been
+// taken apart.  Tiles of 224 and 256 rows keep four registers in scratch memory.
 //
 // What the tile is chosen by is LDS traffic: per 128 channels a wave of 128 x 128 reads 32 KiB for 64 MFMAs of 32 cycles, so
 // the four waves and the arriving 64 KiB take about 1500 of the 2048 cycles that the matrix pipes work; 64 x 64 to a wave would
