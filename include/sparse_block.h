@@ -131,7 +131,8 @@ int sparse_block_norm_backward(const sparse_block_norm_backward_args* args, void
  *   inv_freq            HOST, R / 2 finite doubles, radians per unit of position; NULL: those of sparse_rotary_frequencies
  *                       for theta
  * Strides are in elements (64 bits), multiples of 8; tensors 16-byte aligned.  Results must not overlap qkv or each other.
- * Supported: D in {32, 64, 128, 256}; at most 2^20 heads_q and heads_kv; 1 to 4 axes; R <= D, with halves = 1 a multiple of 8.
+ * Supported: D in {32, 64, 128, 256}; at most 2^20 heads_q and heads_kv, and B L D < 2^35; 1 to 4 axes; R <= D, with
+ * halves = 1 a multiple of 8.
  */
 typedef struct sparse_rotary_args {
   const void* qkv;

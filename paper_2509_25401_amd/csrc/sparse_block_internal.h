@@ -106,6 +106,14 @@ __device__ __forceinline__ int e4m3x4(float a, float b, float c, float d) {
   return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
 
+// A launch has fewer than 2^32 threads along an axis: workgroups beyond kMostBlocks (of up to 1024 threads) go along y.
+constexpr long long kMostBlocks = 1 << 21;
+inline dim3 grid_of(long long blocks) {
+  const long long x = blocks < kMostBlocks ? blocks : kMostBlocks;
+  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+__device__ __forceinline__ long long block_of() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }     // may be past the last one
+
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;

@@ -145,8 +145,8 @@ __global__ void __launch_bounds__(ONE ? 256 : 1024) block_norm_kernel(const Norm
   constexpr Rows ROWS = VEC ? kWhole : (ONE ? NV == 8 : NV == 1) ? kTailApart : kTailMoved;
   __shared__ float slots[2][16][1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long row = ONE ? (long long)blockIdx.x * 4 + wave : (long long)blockIdx.x;
-  if (row >= p.rows) return;                                  // whole waves; with ONE no barrier follows
+  const long long row = ONE ? block_of() * 4 + wave : block_of();
+  if (row >= p.rows) return;                                  // whole waves, and without ONE whole workgroups; with it no barrier follows
   const Place<ROWS> at{ONE ? lane : (int)threadIdx.x, ONE ? 64 : (int)blockDim.x, p.C};
   RowSum<ONE, 1> sum{slots, wave, (int)blockDim.x >> 6};
   const float inv_c = 1.f / (float)p.C;
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(THREADS) block_norm_backward_kernel(const Back
   const int team = wave / waves, base = team * waves;          // the team's first wave
   const Place<ROWS> at{(int)threadIdx.x - base * 64, waves * 64, p.C};
   const float inv_c = 1.f / (float)p.C;
-  const long long chunk = (long long)blockIdx.x * (blockDim.x / 64 / waves) + team, all = p.vectors * p.chunks;
+  const long long chunk = block_of() * (blockDim.x / 64 / waves) + team, all = p.vectors * p.chunks;
   const long long g = min(chunk, all - 1) / p.chunks;
   const long long first = g * p.rows_per_vector + (min(chunk, all - 1) % p.chunks) * p.rows_per_chunk;
   const long long end_g = min(p.rows, (g + 1) * p.rows_per_vector);
@@ -639,9 +639,8 @@ void launch_norm(const NormParams& p, bool vec, bool f8, hipStream_t stream) {
     constexpr int NV = decltype(nv)::value;
     constexpr bool VEC = decltype(v)::value, ONE = decltype(o)::value, F8 = decltype(f)::value;
     if constexpr (!(F8 && !VEC)) {
-      const unsigned grid = (unsigned)(ONE ? (p.rows + 3) / 4 : p.rows);
       const unsigned block = ONE ? 256 : 64 * ((vectors + 64 * NV - 1) / (64 * NV));
-      hipLaunchKernelGGL((block_norm_kernel<TX, TV, NV, VEC, ONE, F8>), dim3(grid), dim3(block), 0, stream, p);
+      hipLaunchKernelGGL((block_norm_kernel<TX, TV, NV, VEC, ONE, F8>), grid_of(ONE ? (p.rows + 3) / 4 : p.rows), dim3(block), 0, stream, p);
     }
   };
   using T = std::true_type;
@@ -667,11 +666,12 @@ template <class TX, class TV>
 void launch_backward(BackParams& p, bool vec, hipStream_t stream) {
   p.row_waves = row_waves(p.C);
   const int teams = teams_of(p.row_waves);
-  const unsigned grid = (unsigned)((p.vectors * p.chunks + teams - 1) / teams), block = 64 * teams * p.row_waves;
+  const dim3 grid = grid_of((p.vectors * p.chunks + teams - 1) / teams);
+  const unsigned block = 64 * teams * p.row_waves;
   auto go = [&](auto nv, auto v, auto threads) {
     constexpr int NV = decltype(nv)::value, THREADS = decltype(threads)::value;
     constexpr bool VEC = decltype(v)::value;
-    hipLaunchKernelGGL((block_norm_backward_kernel<TX, TV, NV, VEC, THREADS>), dim3(grid), dim3(block), 0, stream, p);
+    hipLaunchKernelGGL((block_norm_backward_kernel<TX, TV, NV, VEC, THREADS>), grid, dim3(block), 0, stream, p);
   };
   using T = std::true_type;
   using F = std::false_type;

@@ -876,9 +876,9 @@ struct Route {
 // rows, columns, what a stage costs a CU (us / 100), and how many thirds of a workgroup's time n of them take on one CU:
 // max(3, rate n - less), as they overlap where several fit its LDS
 struct TileCost {
-  int m, n, stage, rate, less;
+  int m, n, stage, rate, less, threads;
 };
-constexpr TileCost kTiles[] = {{128, 128, 64, 3, 0}, {64, 64, 27, 2, 0}, {32, 64, 24, 3, 1}};
+constexpr TileCost kTiles[] = {{128, 128, 64, 3, 0, 512}, {64, 64, 27, 2, 0, 256}, {32, 64, 24, 3, 1, 256}};
 
 constexpr long long kMostSplitTiles = 512;     // tiles times splits, at most
 constexpr int kLeastSplit = 16;                // groups of a split, about
@@ -904,7 +904,7 @@ size_t scratch_of(long long M, long long N, int groups) {
 //     2000 x 9216 x 3072          190       111         84        60 (160 rows; 256: 78)
 //     9001 x 3072 x 256            50        36         28         -
 //     100 x 304 x 9008             22.7      25.8       44         -   in 4 splits 13.6, 13.8, 18.5
-// A large tile's stage does not get cheaper in proportion with its rows (256: 143, 128: 95): below some 200 rows it waits for memory.
+// splits is 0 where there is none, with more results than fit any memory.  A large tile's stage does not get cheaper in proportion with its rows (256: 143, 128: 95): below some 200 rows it waits for memory.
 Route route_of(long long M, long long N, int groups) {
   Route best = {};
   long long best_cost = 1LL << 60;
@@ -914,7 +914,7 @@ Route route_of(long long M, long long N, int groups) {
   for (int t = 0; t < 3; ++t) {
     const TileCost& c = kTiles[t];
     const long long tiles = ceil_div(M, c.m) * ceil_div(N, c.n);
-    if (tiles > 0x3fffffff) continue;
+    if ((tiles + 7) * c.threads > 0xffffffffLL) continue;          // threads of a launch
     // the reduction is split where it is long and the tiles are few: joining costs a launch and the sums' traffic
     const long long most = tiles < 256 ? std::min(kMostSplitTiles / tiles, (long long)groups / kLeastSplit) : 1;
     for (long long splits = 1; splits <= std::max(1LL, most); splits *= 2) {
@@ -976,6 +976,7 @@ int launch_split(const char* who, const GemmParams& p, const Route& r, float* pa
 
 // scratch: scratch_of() bytes, 256-byte aligned
 int launch_gemm(const char* who, const GemmParams& p, const Route& r, uint8_t* scratch, hipStream_t stream) {
+  if (r.splits == 0) return sa_fail(SPARSE_ATTN_ERR_UNSUPPORTED, "%s: too many results, %lld x %lld", who, p.M, p.N);
   if (r.ki == 0)
     switch (r.tile) {
       case 0: return launch_split<128, 128, 4, 2, 3>(who, p, r, (float*)scratch, stream);

@@ -25,6 +25,7 @@ using namespace sa_block;
 
 constexpr int kMaxAxes = 4, kMaxPairs = 128;
 constexpr int kMaxHeads = 1 << 20;     // so that their channels are counted in 32 bits
+constexpr long long kMostGroups = (1 << 24) - 1;     // workgroups of 256 threads: fewer than 2^32 of these
 
 struct RotaryParams {
   const __bf16* qkv;
@@ -457,7 +458,7 @@ int sparse_rotary_heads(const sparse_rotary_args* a, void* hip_stream) {
       if (rows_clash(out[i], out[j], a->B, a->L, a->D)) return sa_fail(SPARSE_ATTN_ERR_INVALID, "%s: %s must not overlap %s", who, out[i].name, out[j].name);
   const int per_group = 4 * 512 / a->D;
   const long long groups = (p.tokens + per_group - 1) / per_group;
-  if (groups > 0x7fffffffLL) return sa_fail(SPARSE_ATTN_ERR_UNSUPPORTED, "%s: too many tokens", who);
+  if (groups > kMostGroups) return sa_fail(SPARSE_ATTN_ERR_UNSUPPORTED, "%s: too many tokens", who);
   const int parts = head_parts(groups, heads);
   p.heads_per_part = (heads + parts - 1) / parts;
   const dim3 grid((unsigned)groups, (unsigned)((heads + p.heads_per_part - 1) / p.heads_per_part));
@@ -499,7 +500,7 @@ int sparse_rotary_heads_backward(const sparse_rotary_args* a, void* dqkv, long l
   const bool sums = dq_weight || dk_weight;
   // with sums a workgroup takes several token groups, so that there are few of them to add and to keep (33024 tokens, 72 heads
   // of 128: 326 us, with 512 workgroups 364, with one for each group 328)
-  const long long most = sums ? 2048 : 0x7fffffffLL;
+  const long long most = sums ? 2048 : kMostGroups;
   const long long groups = all < most ? all : most;
   const int parts = head_parts(groups, heads);
   p.heads_per_part = (heads + parts - 1) / parts;

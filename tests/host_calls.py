@@ -35,7 +35,7 @@ _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes
 
 
 def at(n):
-    return (n + 1) << 42
+    return (n + 1) << 47
 
 
 class Library:
