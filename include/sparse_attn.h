@@ -332,9 +332,10 @@ int sparse_attn_profile_end(int* calls, double* plan_ms_total, double* attn_ms_t
  * Scratch memory of the one-shot calls.  sparse_attn_fwd, sparse_attn_fwd_stream, sparse_attn_fwd_timed,
  * sparse_attn_fwd_forecast and sparse_symbols_update* keep one device buffer per (device, stream) inside the
  * library: allocated on the first call on that stream (hipMalloc), grown when a later call needs more (stream
- * synchronisation + hipFree + hipMalloc), shared by all of these calls on the stream and those of sparse_block.h, never shrunk.  Consequences:
- * calls of several host threads on one stream wait for each other (while the other's kernels are enqueued, not while they
- * run); such a call can be captured into a HIP graph only after a call of at least the same size has run on that stream,
+ * synchronisation + hipFree + hipMalloc), shared by all of these calls on the stream and those of sparse_block.h, never
+ * shrunk.  Consequences: calls of several host threads on one stream wait for each other (while the other's kernels are
+ * enqueued, not while they run); such a call can be captured into a HIP graph only after a call of at least the same size
+ * has run on that stream,
  * and a graph captured from it becomes invalid if the buffer grows afterwards; the plan calls, sparse_attn_fwd_noalloc
  * and sparse_attn_fwd_workspace have no such restriction.  sparse_attn_release_scratch waits for the stream and frees
  * its buffer (call it before destroying a stream: the library cannot see that a stream handle has died, and a

@@ -47,8 +47,8 @@ extern "C" {
  *              NULL for zeros (scale, shift) and ones (gate)
  * x, y, x_out and h are contiguous.  None of the results may overlap another argument, but x_out may be x.
  * Supported: 1 <= channels <= 16384; with E4M3 a multiple of 16, and 16-byte aligned x, y, x_out, h and vectors (8-byte
- * aligned h).  Other tensors need the alignment of their elements alone; rows that do not start on 16
- * bytes, or are no multiple of 8 channels, move in the same runs of eight values, and slower.
+ * aligned h).  Other tensors need the alignment of their elements alone; rows that do not start on 16 bytes, or are no
+ * multiple of 8 channels, move in the same runs of eight values, and slower.
  */
 typedef struct sparse_block_norm_args {
   const void* x;
@@ -82,8 +82,8 @@ int sparse_block_norm(const sparse_block_norm_args* args, void* hip_stream);
  *   dweight, dpost_weight      device, fp32 [channels], or NULL: summed over all rows
  *   dscale, dshift, dgate      device, fp32 [ceil(rows / rows_per_vector), channels] contiguous, or NULL: summed over the
  *             rows of a vector.  Sums are fp32 in an order that depends on the sizes alone.
- * Uses the per-stream scratch buffer for the sums that are asked for: a float for each channel and chunk of rows, some 2000
- * chunks or one to a vector, and two more for each vector and channel where dweight and dpost_weight are wanted.
+ * Uses the per-stream scratch buffer for the sums that are asked for: a float for each channel and chunk of rows, up to some
+ * thousands of chunks (none with one to a vector), and one more for each vector and channel for dweight and for dpost_weight.
  * Everything else as for sparse_block_norm.
  */
 typedef struct sparse_block_norm_backward_args {

@@ -384,9 +384,9 @@ def sparse_fp8_quantize(x, q=None, q_scales=None, qt=None, qt_scales=None, block
     """8-bit form of x (bf16 [R,C]): e4m3 values and exponent bytes, q * 2^(scale - 127), for groups of 128.
 
     q float8_e4m3fn [R,C] with q_scales uint8 [R,ceil(C/128)] (groups along a row), and / or the transposed form qt [C,R] with
-    qt_scales [C,ceil(R/128)] (groups along the rows of x; the rows of qt lie at a multiple of 16 bytes, which may be further apart than
-    R, and are written up to the next such multiple behind R, zeros from R on: torch.empty(C, -(-R//16)*16)[:, :R]).  block=True: groups of 128 x 128, scales [ceil(R/128),ceil(C/128)] and transposed.  Returns (q, q_scales, qt,
-    qt_scales)."""
+    qt_scales [C,ceil(R/128)] (groups along the rows of x; the rows of qt start at multiples of 16 bytes, further apart than R if
+    need be, and are written up to the next such multiple behind R, zeros from R on: torch.empty(C, -(-R//16)*16)[:, :R]).
+    block=True: groups of 128 x 128, scales [ceil(R/128),ceil(C/128)] and transposed.  Returns (q, q_scales, qt, qt_scales)."""
     lib = _lib or _library()
     if x is None or x.dim() != 2:
         raise ValueError("x must be [R, C]")
